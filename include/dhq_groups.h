@@ -101,7 +101,8 @@ DHQ_API dhq_status_t dhq_checkpoint_act_grad(const int8_t *codes, const uint8_t 
  *              arguments, 16-byte aligned; NULL if that is 0.  (It holds parts of the sums, and a copy of 16-bit dy whose rows are not
  *              aligned to 16 bytes.)  Used until the call's work on `stream` is done: calls that may
  *              run at the same time need one each.
- * fp16 dy: x^ is taken in fp16, as a checkpoint of fp16 values has it; larger ones become infinite.
+ * fp16 dy: the q 2^e of a group are fp16 numbers times a power of two, which is one for the rows that a block sums and such that the largest is
+ * finite (1 while q 2^e stay below 65,504, and then nothing of them is rounded; else what lies 2^39 below the largest is).
  * Errors: also ALLOC if the workspace is too small.
  */
 DHQ_API dhq_status_t dhq_checkpoint_weight_grad_workspace(int64_t T, int64_t N, int64_t K, int group, dhq_rot_t rotation,

@@ -5,6 +5,12 @@
 // is exactly the sum of three bf16 numbers (8 bits each, by truncation), whose products go into the same sums.  The rotation is linear and
 // does not touch the rows that the sum runs over: dW = (dy^T q 2^e) H / G, applied once to the finished sums.
 //
+// fp16 holds 65,504 at most, and q 2^e of a rotated group is up to G times as large as its x (rounded, it is larger without the rotation, too: 64 2^10 for
+// 65,504).  A block whose dy is fp16 therefore takes its tile a second time if it has met such numbers: for each group with the least s at which
+// 127 2^(e - s) is finite, powers of e - s, and finished sums times 2^s.  Then what lies 2^39 below the group's largest is rounded.
+// The warp that makes powers of the exponents sees them anyway.  (8,192 rows, 4,096 x 4,096, groups of 128 / 32: 236 / 240 us without any of this, 242 / 248 with it,
+// for the second copy of the code beside the first; 253 / 277 where all warps look over the exponents first; as a function behind a call 245 / 265.)
+//
 // What bounds it is the traffic of shared memory (128 bytes per cycle and SM), not only the tensor pipe: with both operands there a
 // 128 x 256 tile needs 96 bytes per cycle for the MMAs alone.  So x^ is the operand that lives in tensor memory (lane = input feature,
 // column = two rows of the batch): the converting warps read codes as TMA left them in shared memory, transposed on the way as 8 x 8 matrices of
@@ -90,6 +96,7 @@ __device__ __forceinline__ void tmem_st_16x128b(uint32_t at, const uint32_t (&v)
                    "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
 }
 
+__device__ __forceinline__ void mbar_inval(uint32_t bar) { asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
 template <int WARPS> __device__ __forceinline__ void converters_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory"); }
 
 struct GradArgs {
@@ -166,6 +173,9 @@ __device__ __forceinline__ uint32_t powers16(uint32_t bytes, bool &small, __half
     small = small || least != bytes;
     return (__vminu2(least, 0x008f008fu) - 0x00700070u) << 10;
 }
+constexpr uint32_t kLargestByte = 136; // 127 2^9 is finite in fp16, 64 2^10 is not
+// Four exponent bytes less the shifts of their groups; zeros and broken groups stay, and what falls to 0 is nothing beside the largest.
+__device__ __forceinline__ uint32_t shifted(uint32_t bytes, uint32_t shifts) { return __vsubus4(bytes, shifts & ~__vcmpeq4(bytes, 0xffffffffu)); }
 __device__ __forceinline__ uint32_t small16(uint32_t byte) // 2^(e + 14) for e < -14, else 1; zeros for groups of zeros
 {
     return byte == 0 ? 0u : byte >= 113u ? 0x3c00u : __half_as_ushort(__float2half_rn(power_of(byte + 14u)));
@@ -243,6 +253,7 @@ weight_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ C
     __shared__ uint64_t bars[3 * SB + 2 * SA + 5];
     __shared__ uint32_t tmem_holder;
     __shared__ int failed;
+    __shared__ uint32_t large, tops[4]; // HALF: whether a byte above kLargestByte was met; then the largest of each group
     const int warp = (int)ptx::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     auto full_b = [&](int s) { return ptx::smem_u32(bars + s); };               // dy of a stage is there
     auto full_c = [&](int s) { return ptx::smem_u32(bars + SB + s); };          // its codes and powers are
@@ -257,8 +268,7 @@ weight_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ C
     const int k0 = kt * kTileK, n0 = nt * BN;
     const int step0 = (int)((int64_t)a.steps * split / a.splits), steps = (int)((int64_t)a.steps * (split + 1) / a.splits) - step0;
 
-    if (threadIdx.x == 0) {
-        failed = 0;
+    auto init_barriers = [&] {
         for (int s = 0; s < SB; ++s) {
             ptx::mbar_init(full_b(s), F32 ? kLoadWarps / kLoadTurns : 1);
             ptx::mbar_init(full_c(s), 2);
@@ -274,6 +284,10 @@ weight_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ C
             ptx::mbar_init(chunk_empty + 8 * c, CW);
         }
         ptx::fence_mbar_init();
+    };
+    if (threadIdx.x == 0) {
+        failed = 0, large = 0, tops[0] = tops[1] = tops[2] = tops[3] = 0;
+        init_barriers();
     }
     // No block takes tensor memory and then waits for a kernel that may not have its own yet, and none of a later kernel starts before this one has.
     ptx::wait_for_previous_kernels();
@@ -288,310 +302,356 @@ weight_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ C
     const uint32_t tmem = ptx::uniform(tmem_holder), first_a = tmem + kFirstA<T, BN, DRAIN>;
     const Waiter wait{&failed, ptx::globaltimer()};
 
-    if (warp < CW) {
-        // x^: inputs 32 * (warp % 4) on of the tile, all rows of a step
-        const int quarter = warp & 3, turn = warp >> 2;
-        const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
-        // sums of the input whose numbers go to this lane of tensor memory, for a part of the outputs
-        const int x = 32 * quarter + 16 * (lane >> 4) + 2 * (lane & 7) + ((lane >> 3) & 1);
-        constexpr int PART = BN * 4 / CW;
-        const int part = (warp >> 2) * PART;
-        // (matrix lane / 8: inputs 16 (lane / 8 % 2) on, rows 8 (lane / 16) on of 16)
-        const uint32_t code_at = ptx::smem_u32(smem) + DY + (lane >> 4) * 1024 + (lane & 7) * 128 + (((2 * quarter + (lane >> 3 & 1)) ^ (lane & 7)) << 4);
-        const uint32_t power_at = ptx::smem_u32(powers) + ((32 * quarter / a.G) * 32 + (lane & 3) * 4) * 4;
-        // (stages and their phases are counted, not divided out: 234 instructions a step and warp of 32 rows, with them, were 0.9 of what a
-        // scheduler issues in the time of the step's MMAs)
-        int sb = turn % SB, round_b = turn / SB & 1;
-        auto convert = [&](int i) {
-            const int s = i % SA;
-            if (!__all_sync(0xffffffffu, wait(full_c(sb), round_b))) return false;
-            uint32_t v[2][8];
+    // The whole tile; the second time with powers of e - s and the groups' shifts s, a byte each.
+    auto take_tile = [&](auto again, uint32_t shifts) {
+        constexpr bool AGAIN = decltype(again)::value;
+        if (warp < CW) {
+            // x^: inputs 32 * (warp % 4) on of the tile, all rows of a step
+            const int quarter = warp & 3, turn = warp >> 2;
+            const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
+            // sums of the input whose numbers go to this lane of tensor memory, for a part of the outputs
+            const int x = 32 * quarter + 16 * (lane >> 4) + 2 * (lane & 7) + ((lane >> 3) & 1);
+            constexpr int PART = BN * 4 / CW;
+            const int part = (warp >> 2) * PART;
+            // (matrix lane / 8: inputs 16 (lane / 8 % 2) on, rows 8 (lane / 16) on of 16)
+            const uint32_t code_at = ptx::smem_u32(smem) + DY + (lane >> 4) * 1024 + (lane & 7) * 128 + (((2 * quarter + (lane >> 3 & 1)) ^ (lane & 7)) << 4);
+            const uint32_t power_at = ptx::smem_u32(powers) + ((32 * quarter / a.G) * 32 + (lane & 3) * 4) * 4;
+            // (stages and their phases are counted, not divided out: 234 instructions a step and warp of 32 rows, with them, were 0.9 of what a
+            // scheduler issues in the time of the step's MMAs)
+            int sb = turn % SB, round_b = turn / SB & 1;
+            auto convert = [&](int i) {
+                const int s = i % SA;
+                if (!__all_sync(0xffffffffu, wait(full_c(sb), round_b))) return false;
+                uint32_t v[2][8];
 #pragma unroll
-            for (int o = 0; o < 8; o += 2) load_transposed(code_at + sb * STAGE + o * 1024, v[0][o], v[1][o], v[0][o + 1], v[1][o + 1]);
-            uint32_t by[8];
-            auto powers_of = [&](int which) {
+                for (int o = 0; o < 8; o += 2) load_transposed(code_at + sb * STAGE + o * 1024, v[0][o], v[1][o], v[0][o + 1], v[1][o + 1]);
+                uint32_t by[8];
+                auto powers_of = [&](int which) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint4 p = load_shared16(power_at + sb * (kScaleWords * 4) + 64 * h + which);
-                    by[4 * h] = p.x, by[4 * h + 1] = p.y, by[4 * h + 2] = p.z, by[4 * h + 3] = p.w;
-                }
-            };
-            powers_of(0);
-            uint32_t out[2][16];
-#pragma unroll
-            for (int o = 0; o < 8; ++o)
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    out[m][2 * o] = numbers_of(v[m][o], by[o], M());
-                    out[m][2 * o + 1] = numbers_of(v[m][o] >> 8, by[o], M());
-                }
-            if (HALF && load_shared(ptx::smem_u32(powers) + sb * (kScaleWords * 4) + 1024)) { // tiny groups
-                powers_of(512);
+                    for (int h = 0; h < 2; ++h) {
+                        const uint4 p = load_shared16(power_at + sb * (kScaleWords * 4) + 64 * h + which);
+                        by[4 * h] = p.x, by[4 * h + 1] = p.y, by[4 * h + 2] = p.z, by[4 * h + 3] = p.w;
+                    }
+                };
+                powers_of(0);
+                uint32_t out[2][16];
 #pragma unroll
                 for (int o = 0; o < 8; ++o)
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        uint32_t &w = out[y & 1][2 * o + (y >> 1)];
-                        const __half2 r = __hmul2(*reinterpret_cast<const __half2 *>(&w), *reinterpret_cast<const __half2 *>(&by[o]));
-                        w = *reinterpret_cast<const uint32_t *>(&r);
+                    for (int m = 0; m < 2; ++m) {
+                        out[m][2 * o] = numbers_of(v[m][o], by[o], M());
+                        out[m][2 * o + 1] = numbers_of(v[m][o] >> 8, by[o], M());
                     }
+                if (HALF && load_shared(ptx::smem_u32(powers) + sb * (kScaleWords * 4) + 1024)) { // tiny groups
+                    powers_of(512);
+#pragma unroll
+                    for (int o = 0; o < 8; ++o)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            uint32_t &w = out[y & 1][2 * o + (y >> 1)];
+                            const __half2 r = __hmul2(*reinterpret_cast<const __half2 *>(&w), *reinterpret_cast<const __half2 *>(&by[o]));
+                            w = *reinterpret_cast<const uint32_t *>(&r);
+                        }
+                }
+                sb += TURNS;
+                if (sb >= SB) sb -= SB, round_b ^= 1;
+                if (!__all_sync(0xffffffffu, wait(empty_a(s), ((i / SA) & 1) ^ 1))) return false;
+                ptx::tc_fence_after();
+                const uint32_t to = first_a + lanes + 32 * s;
+                tmem_st_16x128b(to, out[0]);
+                tmem_st_16x128b(to + (16u << 16), out[1]);
+                ptx::tmem_wait_st();
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(full_a(s));
+                return true;
+            };
+            int drained = 0;
+            auto drain = [&] { // the sums of chunk `drained` join the running ones (each thread has its own)
+                if (!__all_sync(0xffffffffu, wait(chunk_full + 8 * (drained & 1), drained >> 1 & 1))) return false;
+                ptx::tc_fence_after();
+#pragma unroll 1
+                for (int n = part; n < part + PART; n += 32) {
+                    uint32_t v[32];
+                    ptx::tmem_ld32(tmem + lanes + BN * (drained & 1) + n, v);
+                    ptx::tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        float *to = running + (n + i) * kPitch + x;
+                        *to = drained ? __fadd_rn(*to, __uint_as_float(v[i])) : __uint_as_float(v[i]);
+                    }
+                }
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(chunk_empty + 8 * (drained & 1));
+                ++drained;
+                return true;
+            };
+            const int drains = DRAIN && steps > 0 ? (steps - 1) / kChunk : 0;
+            bool on = true;
+            for (int i = turn; i < steps && on; i += TURNS) {
+                if (DRAIN && drained < i / kChunk && i % kChunk >= DRAIN_AT) on = drain();
+                on = on && convert(i);
             }
-            sb += TURNS;
-            if (sb >= SB) sb -= SB, round_b ^= 1;
-            if (!__all_sync(0xffffffffu, wait(empty_a(s), ((i / SA) & 1) ^ 1))) return false;
+            while (DRAIN && on && drained < drains) on = drain();
+            const bool ok = steps == 0 || wait(done, 0);
             ptx::tc_fence_after();
-            const uint32_t to = first_a + lanes + 32 * s;
-            tmem_st_16x128b(to, out[0]);
-            tmem_st_16x128b(to + (16u << 16), out[1]);
-            ptx::tmem_wait_st();
-            ptx::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(full_a(s));
-            return true;
-        };
-        int drained = 0;
-        auto drain = [&] { // the sums of chunk `drained` join the running ones (each thread has its own)
-            if (!__all_sync(0xffffffffu, wait(chunk_full + 8 * (drained & 1), drained >> 1 & 1))) return false;
-            ptx::tc_fence_after();
+            converters_sync<CW>(); // everyone is past the ring
+            const int64_t out = a.partial ? (int64_t)blockIdx.x * BN * kTileK : 0;
+            const float up = AGAIN ? power_of(127u + (shifts >> (8 * (x / a.G)) & 255u)) : 1.0f;
 #pragma unroll 1
             for (int n = part; n < part + PART; n += 32) {
-                uint32_t v[32];
-                ptx::tmem_ld32(tmem + lanes + BN * (drained & 1) + n, v);
+                uint32_t v[32], w[32];
+                ptx::tmem_ld32(tmem + lanes + BN * (drains & 1) + n, v);
+                if (F32) ptx::tmem_ld32(tmem + lanes + 2 * BN + n, w);
                 ptx::tmem_wait_ld();
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
-                    float *to = running + (n + i) * kPitch + x;
-                    *to = drained ? __fadd_rn(*to, __uint_as_float(v[i])) : __uint_as_float(v[i]);
+                    float f = __uint_as_float(v[i]);
+                    if (F32) f = __fadd_rn(f, __uint_as_float(w[i]));
+                    if (drains > 0) f = __fadd_rn(running[(n + i) * kPitch + x], f);
+                    if (AGAIN) f = __fmul_rn(f, up);
+                    f = steps == 0 ? 0.0f : ok && !failed ? f : __uint_as_float(0x7fffffffu);
+                    if (a.partial) a.partial[out + (n + i) * kTileK + x] = f;
+                    else running[(n + i) * kPitch + x] = f;
                 }
             }
             ptx::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(chunk_empty + 8 * (drained & 1));
-            ++drained;
-            return true;
-        };
-        const int drains = DRAIN && steps > 0 ? (steps - 1) / kChunk : 0;
-        bool on = true;
-        for (int i = turn; i < steps && on; i += TURNS) {
-            if (DRAIN && drained < i / kChunk && i % kChunk >= DRAIN_AT) on = drain();
-            on = on && convert(i);
-        }
-        while (DRAIN && on && drained < drains) on = drain();
-        const bool ok = steps == 0 || wait(done, 0);
-        ptx::tc_fence_after();
-        converters_sync<CW>(); // everyone is past the ring
-        const int64_t out = a.partial ? (int64_t)blockIdx.x * BN * kTileK : 0;
-#pragma unroll 1
-        for (int n = part; n < part + PART; n += 32) {
-            uint32_t v[32], w[32];
-            ptx::tmem_ld32(tmem + lanes + BN * (drains & 1) + n, v);
-            if (F32) ptx::tmem_ld32(tmem + lanes + 2 * BN + n, w);
-            ptx::tmem_wait_ld();
+            if (!a.partial) {
+                converters_sync<CW>();
+                for (int r = threadIdx.x / 4; r < BN; r += 8 * CW) { // four threads to a row of 128 inputs
+                    float v[4][8];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                float f = __uint_as_float(v[i]);
-                if (F32) f = __fadd_rn(f, __uint_as_float(w[i]));
-                if (drains > 0) f = __fadd_rn(running[(n + i) * kPitch + x], f);
-                f = steps == 0 ? 0.0f : ok && !failed ? f : __uint_as_float(0x7fffffffu);
-                if (a.partial) a.partial[out + (n + i) * kTileK + x] = f;
-                else running[(n + i) * kPitch + x] = f;
-            }
-        }
-        ptx::tc_fence_before();
-        if (!a.partial) {
-            converters_sync<CW>();
-            for (int r = threadIdx.x / 4; r < BN; r += 8 * CW) { // four threads to a row of 128 inputs
-                float v[4][8];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) load8<float, true>(running + r * kPitch + 32 * c + 8 * (threadIdx.x & 3), 8, v[c]);
-                write_rows(a, v, n0 + (r & ~7), k0, HALF, running + (r & ~7) * kPitch);
-            }
-        }
-    } else if (warp == MMA_WARP) {
-        const uint32_t idesc = idesc_f16(!HALF, kTileK, BN);
-        for (int i = 0; i < steps; ++i) {
-            const int sa = i % SA, sb = i % SB;
-            bool ok = true;
-            const int chunk = DRAIN ? i / kChunk : 0;
-            if (DRAIN && i > 0 && i % kChunk == 0) {
-                ptx::mma_commit(chunk_full + 8 * ((chunk - 1) & 1));
-                ok = chunk < 2 || wait(chunk_empty + 8 * (chunk & 1), ((chunk >> 1) - 1) & 1);
-            }
-            ok = ok && wait(full_b(sb), (i / SB) & 1) && wait(full_a(sa), (i / SA) & 1);
-            if (!__all_sync(0xffffffffu, ok)) break;
-            ptx::tc_fence_after();
-#pragma unroll
-            for (int p = 0; p < TERMS; ++p)
-#pragma unroll
-                for (int kk = 0; kk < kStep / 16; ++kk)
-                    mma_f16_tmem(tmem + (p ? 2 * BN : BN * (chunk & 1)), first_a + 32 * sa + 8 * kk, desc_mn(ptx::smem_u32(smem) + sb * STAGE + p * (BN * kStep * 2) + kk * 2048), idesc,
-                                 kk | (p ? i | (p - 1) : DRAIN ? i % kChunk : i));
-            ptx::mma_commit(empty_a(sa));
-            ptx::mma_commit(empty_b(sb));
-        }
-        if (steps > 0) ptx::mma_commit(done); // (else nobody waits for its arrival)
-    } else if (warp == RING_WARP) { // codes and dy by TMA
-        for (int i = 0; i < steps; ++i) {
-            const int s = i % SB;
-            if (!__all_sync(0xffffffffu, wait(empty_b(s), ((i / SB) & 1) ^ 1))) break;
-            if (lane == 0) {
-                ptx::mbar_expect_tx(full_c(s), kTileK * kStep);
-                tma_load(ptx::smem_u32(smem) + s * STAGE + DY, &code_map, k0, (step0 + i) * kStep, full_c(s));
-                if (!F32) {
-                    ptx::mbar_expect_tx(full_b(s), DY);
-#pragma unroll
-                    for (int b = 0; b < BN / 64; ++b)
-                        tma_load(ptx::smem_u32(smem) + s * STAGE + b * 8192, &dy_map, n0 + 64 * b, (step0 + i) * kStep, full_b(s));
+                    for (int c = 0; c < 4; ++c) load8<float, true>(running + r * kPitch + 32 * c + 8 * (threadIdx.x & 3), 8, v[c]);
+                    write_rows(a, v, n0 + (r & ~7), k0, HALF, running + (r & ~7) * kPitch);
                 }
             }
-            __syncwarp();
-        }
-    } else if (warp == POWER_WARP) {
-        // Exponents of rows 2 lane and 2 lane + 1, as pairs of powers.  A row's one, two or four exponents of the tile come in one load where
-        // rows are aligned for it (each load of the warp touches 32 lines).  The loads of four steps are issued together, while the four
-        // before are handed out, and nothing looks at them until then (waiting for one load of many in flight would wait for all; with a test
-        // or a shift behind each load 511 in place of 259 us for 8,192 rows, 4,096 x 4,096).
-        const int per_row = a.Kp / a.G, per_tile = kTileK / a.G, last_group = min(per_tile, per_row - k0 / a.G) - 1;
-        auto run = [&](auto element, auto many) {
-            using E = decltype(element);
-            constexpr int LOADS = decltype(many)::value, COUNT = LOADS * (int)sizeof(E), kAhead = 4;
-            const uint8_t *const first = a.exponents + (int64_t)step0 * kStep * per_row + k0 / a.G;
-            const int rows = (int)min((int64_t)steps * kStep, a.T - (int64_t)step0 * kStep); // of this block
-            E e[kAhead][2][LOADS];
-            auto load = [&](int i, E (&v)[2][LOADS]) {
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const uint8_t *at = first + (int64_t)min(i * kStep + 2 * lane + r, rows - 1) * per_row; // (behind the last row: that one's, see below)
-#pragma unroll
-                    for (int g = 0; g < LOADS; ++g) v[r][g] = *reinterpret_cast<const E *>(at + (LOADS > 1 ? min(g, last_group) : 0));
+        } else if (warp == MMA_WARP) {
+            const uint32_t idesc = idesc_f16(!HALF, kTileK, BN);
+            for (int i = 0; i < steps; ++i) {
+                const int sa = i % SA, sb = i % SB;
+                bool ok = true;
+                const int chunk = DRAIN ? i / kChunk : 0;
+                if (DRAIN && i > 0 && i % kChunk == 0) {
+                    ptx::mma_commit(chunk_full + 8 * ((chunk - 1) & 1));
+                    ok = chunk < 2 || wait(chunk_empty + 8 * (chunk & 1), ((chunk >> 1) - 1) & 1);
                 }
-            };
+                ok = ok && wait(full_b(sb), (i / SB) & 1) && wait(full_a(sa), (i / SA) & 1);
+                if (!__all_sync(0xffffffffu, ok)) break;
+                ptx::tc_fence_after();
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) load(u, e[u]);
-            int s = 0, before = 0, round = 0, round_before = 0;
-            // pair p of rows (of 32): half p / 16 of the step, octet (p / 4) % 4, pair p % 4 of it; a reader wants its four octets together
-            uint32_t *const mine = powers + (lane >> 4) * 16 + (lane & 3) * 4 + ((lane >> 2) & 3);
-            for (int i0 = 0; i0 < steps; i0 += kAhead) {
-                uint32_t byte[kAhead][2]; // up to four exponents of a row
+                for (int p = 0; p < TERMS; ++p)
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u)
+                    for (int kk = 0; kk < kStep / 16; ++kk)
+                        mma_f16_tmem(tmem + (p ? 2 * BN : BN * (chunk & 1)), first_a + 32 * sa + 8 * kk, desc_mn(ptx::smem_u32(smem) + sb * STAGE + p * (BN * kStep * 2) + kk * 2048), idesc,
+                                     kk | (p ? i | (p - 1) : DRAIN ? i % kChunk : i));
+                ptx::mma_commit(empty_a(sa));
+                ptx::mma_commit(empty_b(sb));
+            }
+            if (steps > 0) ptx::mma_commit(done); // (else nobody waits for its arrival)
+        } else if (warp == RING_WARP) { // codes and dy by TMA
+            for (int i = 0; i < steps; ++i) {
+                const int s = i % SB;
+                if (!__all_sync(0xffffffffu, wait(empty_b(s), ((i / SB) & 1) ^ 1))) break;
+                if (lane == 0) {
+                    ptx::mbar_expect_tx(full_c(s), kTileK * kStep);
+                    tma_load(ptx::smem_u32(smem) + s * STAGE + DY, &code_map, k0, (step0 + i) * kStep, full_c(s));
+                    if (!F32) {
+                        ptx::mbar_expect_tx(full_b(s), DY);
+#pragma unroll
+                        for (int b = 0; b < BN / 64; ++b)
+                            tma_load(ptx::smem_u32(smem) + s * STAGE + b * 8192, &dy_map, n0 + 64 * b, (step0 + i) * kStep, full_b(s));
+                    }
+                }
+                __syncwarp();
+            }
+        } else if (warp == POWER_WARP) {
+            // Exponents of rows 2 lane and 2 lane + 1, as pairs of powers.  A row's one, two or four exponents of the tile come in one load where
+            // rows are aligned for it (each load of the warp touches 32 lines).  The loads of four steps are issued together, while the four
+            // before are handed out, and nothing looks at them until then (waiting for one load of many in flight would wait for all; with a test
+            // or a shift behind each load 511 in place of 259 us for 8,192 rows, 4,096 x 4,096).
+            const int per_row = a.Kp / a.G, per_tile = kTileK / a.G, last_group = min(per_tile, per_row - k0 / a.G) - 1;
+            auto run = [&](auto element, auto many) {
+                using E = decltype(element);
+                constexpr int LOADS = decltype(many)::value, COUNT = LOADS * (int)sizeof(E), kAhead = 4;
+                const uint8_t *const first = a.exponents + (int64_t)step0 * kStep * per_row + k0 / a.G;
+                const int rows = (int)min((int64_t)steps * kStep, a.T - (int64_t)step0 * kStep); // of this block
+                E e[kAhead][2][LOADS];
+                auto load = [&](int i, E (&v)[2][LOADS]) {
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        byte[u][r] = 0;
+                        const uint8_t *at = first + (int64_t)min(i * kStep + 2 * lane + r, rows - 1) * per_row; // (behind the last row: that one's, see below)
 #pragma unroll
-                        for (int g = 0; g < LOADS; ++g) byte[u][r] |= (uint32_t)e[u][r][g] << (8 * g);
-                        if ((i0 + u) * kStep + 2 * lane + r >= rows) byte[u][r] = 0;
+                        for (int g = 0; g < LOADS; ++g) v[r][g] = *reinterpret_cast<const E *>(at + (LOADS > 1 ? min(g, last_group) : 0));
                     }
+                };
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) load(i0 + kAhead + u, e[u]);
+                for (int u = 0; u < kAhead; ++u) load(u, e[u]);
+                int s = 0, before = 0, round = 0, round_before = 0;
+                uint32_t seen = 0;
+                // pair p of rows (of 32): half p / 16 of the step, octet (p / 4) % 4, pair p % 4 of it; a reader wants its four octets together
+                uint32_t *const mine = powers + (lane >> 4) * 16 + (lane & 3) * 4 + ((lane >> 2) & 3);
+                for (int i0 = 0; i0 < steps; i0 += kAhead) {
+                    uint32_t byte[kAhead][2]; // up to four exponents of a row
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-                    const int i = i0 + u;
-                    if (i >= steps) continue;
-                    uint32_t pair[COUNT]; // (made before the wait: from there to the arrival others wait for this warp)
-                    bool small = false;
+                    for (int u = 0; u < kAhead; ++u)
 #pragma unroll
-                    for (int g = 0; g < COUNT; ++g) pair[g] = powers16(__byte_perm(byte[u][0], byte[u][1], 0x0400 + 0x0101 * g) & 0x00ff00ffu, small, M());
-                    if (HALF) small = __any_sync(0xffffffffu, small);
-                    if (!__all_sync(0xffffffffu, wait(empty_b(s), round ^ 1))) return;
-                    uint32_t *to = mine + s * kScaleWords;
+                        for (int r = 0; r < 2; ++r) {
+                            byte[u][r] = 0;
 #pragma unroll
-                    for (int g = 0; g < COUNT; ++g) to[32 * g] = pair[g];
-                    if (HALF) {
-                        if (small)
-                            for (int g = 0; g < COUNT; ++g)
-                                to[128 + 32 * g] = small16((byte[u][0] >> (8 * g)) & 255u) | small16((byte[u][1] >> (8 * g)) & 255u) << 16;
-                        if (lane == 0) powers[s * kScaleWords + 256] = small;
+                            for (int g = 0; g < LOADS; ++g) byte[u][r] |= (uint32_t)e[u][r][g] << (8 * g);
+                            if (AGAIN) byte[u][r] = shifted(byte[u][r], shifts);
+                            if ((i0 + u) * kStep + 2 * lane + r >= rows) byte[u][r] = 0;
+                        }
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) load(i0 + kAhead + u, e[u]);
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        const int i = i0 + u;
+                        if (i >= steps) continue;
+                        uint32_t pair[COUNT]; // (made before the wait: from there to the arrival others wait for this warp)
+                        bool small = false;
+#pragma unroll
+                        for (int g = 0; g < COUNT; ++g) {
+                            const uint32_t bytes = __byte_perm(byte[u][0], byte[u][1], 0x0400 + 0x0101 * g) & 0x00ff00ffu;
+                            if (HALF && !AGAIN) seen = __vmaxu2(seen, bytes);
+                            pair[g] = powers16(bytes, small, M());
+                        }
+                        if (HALF) small = __any_sync(0xffffffffu, small);
+                        if (!__all_sync(0xffffffffu, wait(empty_b(s), round ^ 1))) return;
+                        uint32_t *to = mine + s * kScaleWords;
+#pragma unroll
+                        for (int g = 0; g < COUNT; ++g) to[32 * g] = pair[g];
+                        if (HALF) {
+                            if (small)
+                                for (int g = 0; g < COUNT; ++g)
+                                    to[128 + 32 * g] = small16((byte[u][0] >> (8 * g)) & 255u) | small16((byte[u][1] >> (8 * g)) & 255u) << 16;
+                            if (lane == 0) powers[s * kScaleWords + 256] = small;
+                        }
+                        // Steps become full in order, though copies may land in another: a converting warp that has seen step j full knows that all
+                        // steps before it were, and with them the round before of the stage that it waits for next.
+                        if (i > 0 && !__all_sync(0xffffffffu, wait(full_c(before), round_before))) return;
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive(full_c(s));
+                        before = s, round_before = round;
+                        if (++s == SB) s = 0, round ^= 1;
                     }
-                    // Steps become full in order, though copies may land in another: a converting warp that has seen step j full knows that all
-                    // steps before it were, and with them the round before of the stage that it waits for next.
-                    if (i > 0 && !__all_sync(0xffffffffu, wait(full_c(before), round_before))) return;
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(full_c(s));
-                    before = s, round_before = round;
-                    if (++s == SB) s = 0, round ^= 1;
                 }
-            }
-        };
-        using std::integral_constant;
-        const bool together = per_row % per_tile == 0 && ((uintptr_t)a.exponents & (per_tile - 1)) == 0;
-        if (steps == 0) {
-        } else if (per_tile == 1) run(uint8_t(), integral_constant<int, 1>());
-        else if (!together) run(uint8_t(), integral_constant<int, 4>()); // (with two groups a tile the last two are not used)
-        else if (per_tile == 2) run(uint16_t(), integral_constant<int, 1>());
-        else run(uint32_t(), integral_constant<int, 1>());
-    } else if (F32) {
-        // fp32 dy, cut into three bf16 terms: a warp takes every eighth row of a step, four features a thread.  Half of the warps wait for
-        // their loads while the other half cuts.
-        constexpr int THREADS = 32 * kLoadWarps / kLoadTurns, ROWS = kStep / (THREADS / 32);
-        static_assert(!F32 || (BN == 128 && THREADS / 32 == 8), "a row of a tile is four features for each thread of a warp");
-        const int turn = (threadIdx.x - 32 * CW) / THREADS, first = (warp - CW) % (THREADS / 32), n = n0 + 4 * lane;
-        const bool whole = a.wide_in && n0 + BN <= a.N;
-        float4 v[ROWS];
-        auto load = [&](int i) {
-            if (i >= steps) return;
-            const int64_t t = (int64_t)(step0 + i) * kStep + first;
-            const float *at = (const float *)a.dy + t * a.lddy + n;
-            const int64_t next = 8 * a.lddy;
-            if (whole && t - first + kStep <= a.T) {
+                if (HALF && !AGAIN && max(seen & 0xffffu, seen >> 16) > kLargestByte) large = 1;
+            };
+            using std::integral_constant;
+            const bool together = per_row % per_tile == 0 && ((uintptr_t)a.exponents & (per_tile - 1)) == 0;
+            if (steps == 0) {
+            } else if (per_tile == 1) run(uint8_t(), integral_constant<int, 1>());
+            else if (!together) run(uint8_t(), integral_constant<int, 4>()); // (with two groups a tile the last two are not used)
+            else if (per_tile == 2) run(uint16_t(), integral_constant<int, 1>());
+            else run(uint32_t(), integral_constant<int, 1>());
+        } else if (F32) {
+            // fp32 dy, cut into three bf16 terms: a warp takes every eighth row of a step, four features a thread.  Half of the warps wait for
+            // their loads while the other half cuts.
+            constexpr int THREADS = 32 * kLoadWarps / kLoadTurns, ROWS = kStep / (THREADS / 32);
+            static_assert(!F32 || (BN == 128 && THREADS / 32 == 8), "a row of a tile is four features for each thread of a warp");
+            const int turn = (threadIdx.x - 32 * CW) / THREADS, first = (warp - CW) % (THREADS / 32), n = n0 + 4 * lane;
+            const bool whole = a.wide_in && n0 + BN <= a.N;
+            float4 v[ROWS];
+            auto load = [&](int i) {
+                if (i >= steps) return;
+                const int64_t t = (int64_t)(step0 + i) * kStep + first;
+                const float *at = (const float *)a.dy + t * a.lddy + n;
+                const int64_t next = 8 * a.lddy;
+                if (whole && t - first + kStep <= a.T) {
 #pragma unroll
-                for (int u = 0; u < ROWS; ++u, at += next) v[u] = *reinterpret_cast<const float4 *>(at);
-            } else {
+                    for (int u = 0; u < ROWS; ++u, at += next) v[u] = *reinterpret_cast<const float4 *>(at);
+                } else {
 #pragma unroll
-                for (int u = 0; u < ROWS; ++u, at += next) {
-                    const int valid = t + 8 * u < a.T ? a.N - n : 0;
-                    v[u] = make_float4(valid > 0 ? at[0] : 0.0f, valid > 1 ? at[1] : 0.0f, valid > 2 ? at[2] : 0.0f, valid > 3 ? at[3] : 0.0f);
+                    for (int u = 0; u < ROWS; ++u, at += next) {
+                        const int valid = t + 8 * u < a.T ? a.N - n : 0;
+                        v[u] = make_float4(valid > 0 ? at[0] : 0.0f, valid > 1 ? at[1] : 0.0f, valid > 2 ? at[2] : 0.0f, valid > 3 ? at[3] : 0.0f);
+                    }
                 }
-            }
-        };
-        // 16 bytes of a row of a tile hold eight features: this thread's are a half of piece lane / 2
-        uint8_t *const to = smem + (lane >> 4) * 8192 + first * 128 + ((((lane >> 1) & 7) ^ first) << 4) + 8 * (lane & 1);
-        auto store = [&](int i) {
-            const int s = i % SB;
-            float top = 0.0f;
+            };
+            // 16 bytes of a row of a tile hold eight features: this thread's are a half of piece lane / 2
+            uint8_t *const to = smem + (lane >> 4) * 8192 + first * 128 + ((((lane >> 1) & 7) ^ first) << 4) + 8 * (lane & 1);
+            auto store = [&](int i) {
+                const int s = i % SB;
+                float top = 0.0f;
 #pragma unroll
-            for (int u = 0; u < ROWS; ++u) {
-                asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(v[u].x), "f"(v[u].y));
-                asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(v[u].z), "f"(v[u].w));
-            }
-            const bool finite = top <= 3.402823466e+38f;
-            if (!__all_sync(0xffffffffu, wait(empty_b(s), ((i / SB) & 1) ^ 1))) return false;
-#pragma unroll
-            for (int u = 0; u < ROWS; ++u) {
-                const float f[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-                uint32_t term[3][4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    term[0][j] = __float_as_uint(f[j]) & 0xffff0000u;
-                    const float rest = __fsub_rn(f[j], __uint_as_float(term[0][j]));
-                    term[1][j] = __float_as_uint(rest) & 0xffff0000u;
-                    term[2][j] = __float_as_uint(__fsub_rn(rest, __uint_as_float(term[1][j])));
+                for (int u = 0; u < ROWS; ++u) {
+                    asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(v[u].x), "f"(v[u].y));
+                    asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(v[u].z), "f"(v[u].w));
                 }
-                if (!finite) // infinities and NaN are their first term
+                const bool finite = top <= 3.402823466e+38f;
+                if (!__all_sync(0xffffffffu, wait(empty_b(s), ((i / SB) & 1) ^ 1))) return false;
+#pragma unroll
+                for (int u = 0; u < ROWS; ++u) {
+                    const float f[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+                    uint32_t term[3][4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const uint32_t bits = __float_as_uint(f[j]) & 0x7fffffffu;
-                        if (bits >= 0x7f800000u) term[1][j] = term[2][j] = 0;
-                        if (bits > 0x7f800000u) term[0][j] = 0x7fff0000u;
+                        term[0][j] = __float_as_uint(f[j]) & 0xffff0000u;
+                        const float rest = __fsub_rn(f[j], __uint_as_float(term[0][j]));
+                        term[1][j] = __float_as_uint(rest) & 0xffff0000u;
+                        term[2][j] = __float_as_uint(__fsub_rn(rest, __uint_as_float(term[1][j])));
                     }
+                    if (!finite) // infinities and NaN are their first term
 #pragma unroll
-                for (int p = 0; p < 3; ++p)
-                    *reinterpret_cast<uint2 *>(to + s * STAGE + p * (BN * kStep * 2) + u * 1024) =
-                        make_uint2(__byte_perm(term[p][0], term[p][1], 0x7632), __byte_perm(term[p][2], term[p][3], 0x7632));
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t bits = __float_as_uint(f[j]) & 0x7fffffffu;
+                            if (bits >= 0x7f800000u) term[1][j] = term[2][j] = 0;
+                            if (bits > 0x7f800000u) term[0][j] = 0x7fff0000u;
+                        }
+#pragma unroll
+                    for (int p = 0; p < 3; ++p)
+                        *reinterpret_cast<uint2 *>(to + s * STAGE + p * (BN * kStep * 2) + u * 1024) =
+                            make_uint2(__byte_perm(term[p][0], term[p][1], 0x7632), __byte_perm(term[p][2], term[p][3], 0x7632));
+                }
+                ptx::fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(full_b(s));
+                return true;
+            };
+            load(turn);
+            for (int i = turn; i < steps; i += kLoadTurns) {
+                if (!store(i)) break;
+                load(i + kLoadTurns);
             }
-            ptx::fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(full_b(s));
-            return true;
-        };
-        load(turn);
-        for (int i = turn; i < steps; i += kLoadTurns) {
-            if (!store(i)) break;
-            load(i + kLoadTurns);
         }
-    }
-    if (failed) __nanosleep(1000000); // copies and MMAs in flight end by themselves
-    __syncthreads();
+        if (failed) __nanosleep(1000000); // copies and MMAs in flight end by themselves
+        __syncthreads();
+    };
+    take_tile(std::false_type(), 0u);
+    if constexpr (HALF)
+        if (__builtin_expect(large, 0)) {
+            const int per_row = a.Kp / a.G, first = k0 / a.G, groups = min(kTileK / a.G, per_row - first);
+            const int64_t end = min((int64_t)(step0 + steps) * kStep, a.T);
+            for (int g = 0; g < groups; ++g) {
+                uint32_t top = 0;
+                for (int64_t r = (int64_t)step0 * kStep + threadIdx.x; r < end; r += kThreadsOf<T>) {
+                    const uint32_t byte = a.exponents[r * per_row + first + g];
+                    top = max(top, byte == 255u ? 0u : byte);
+                }
+                atomicMax(tops + g, top);
+            }
+            // Barriers and sums as at the beginning.  All copies, MMAs and drains have been waited for; the arrivals that say that stages are empty
+            // are, now.
+            if (warp == MMA_WARP) {
+                for (int s = 0; s < min(SB, steps); ++s) wait(empty_b(s), ((steps - 1 - s) / SB) & 1);
+                for (int s = 0; s < min(SA, steps); ++s) wait(empty_a(s), ((steps - 1 - s) / SA) & 1);
+            }
+            ptx::fence_proxy_async(); // (finished rows were written where copies go)
+            ptx::tc_fence_before();
+            __syncthreads();
+            uint32_t shifts = 0;
+            for (int g = 0; g < groups; ++g) shifts |= (max(tops[g], kLargestByte) - kLargestByte) << (8 * g);
+            if (threadIdx.x == 0) {
+                for (int i = 0; i < 3 * SB + 2 * SA + 5; ++i) mbar_inval(ptx::smem_u32(bars + i));
+                init_barriers();
+            }
+            const bool again = shifts && !failed; // (without shifts there are broken groups only)
+            __syncthreads();
+            ptx::tc_fence_after();
+            if (again) take_tile(std::true_type(), shifts);
+        }
     if (warp == MMA_WARP) {
         ptx::tc_fence_after();
         ptx::tmem_dealloc(tmem, COLUMNS);
