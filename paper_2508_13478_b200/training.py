@@ -4,6 +4,9 @@ Between forward and backward pass a linear layer keeps its input, and an activat
 of two per group of consecutive features (1 + 1 / group bytes a value in place of 4 or 2).  Gradients with respect to inputs of a
 linear layer need its weights only and are exact; weight gradients and slopes of activations see the checkpoint's values.
 
+Under torch.autocast a linear layer multiplies in autocast's type, forward and backward, as torch's own does; it keeps its input as it came, and
+the gradient of fp32 weights is summed and written in fp32.
+
 A forward and backward pass may be captured into a CUDA graph in torch's way: warmed up on a side stream, with no eager graph of the same
 leaves alive when the capture begins (torch's gradient accumulation would wait for a stream that is not being captured).
 """
@@ -33,6 +36,7 @@ def _rows(t):
 
 class _Linear(torch.autograd.Function):
     @staticmethod
+    @torch.amp.custom_fwd(device_type="cuda")
     def forward(ctx, x, weight, bias, group, rotation):
         x2 = _rows(x)
         ctx.form, ctx.shape = (group, rotation), x.shape
@@ -46,6 +50,7 @@ class _Linear(torch.autograd.Function):
 
     @staticmethod
     @once_differentiable
+    @torch.amp.custom_bwd(device_type="cuda")   # (the products below take the types that the forward pass took)
     def backward(ctx, dy):
         weight, codes, exponents = ctx.saved_tensors
         group, rotation = ctx.form
@@ -53,7 +58,8 @@ class _Linear(torch.autograd.Function):
         dx = (dy2 @ weight).reshape(ctx.shape) if ctx.needs_input_grad[0] else None
         dw = None
         if ctx.needs_input_grad[1]:
-            dw = torch.empty_like(weight, memory_format=torch.contiguous_format)
+            # (16-bit weights under autocast of the other 16-bit type: fp32, which autograd rounds to theirs)
+            dw = torch.empty(weight.shape, dtype=weight.dtype if weight.dtype == dy.dtype else torch.float32, device=weight.device)
             dhq_checkpoint_weight_grad(codes, exponents, dy2, dw, group=group, rotation=rotation)
         db = dy2.sum(0) if ctx.needs_input_grad[2] else None
         return dx, dw, db, None, None
@@ -81,7 +87,7 @@ class _Activation(torch.autograd.Function):
 
 
 def checkpointed_linear(x, weight, bias=None, group=64, rotation=DHQ_ROT_INPUT):
-    """x weight^T + bias (fp32, bf16 or fp16 CUDA tensors of one dtype, x [..., K]), keeping x as an 8-bit checkpoint for the weight's gradient."""
+    """x weight^T + bias (fp32, bf16 or fp16 CUDA tensors, of one dtype unless autocast is on; x [..., K]), keeping x as an 8-bit checkpoint for the weight's gradient."""
     return _Linear.apply(x, weight, bias, group, rotation)
 
 
