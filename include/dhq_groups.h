@@ -78,6 +78,7 @@ DHQ_API dhq_status_t dhq_w4_linear(const uint8_t *codes, const uint16_t *scales,
  *               omega0 and act_s0 (finite; act_s0 > 0 for the wavelet) are ignored by the others.
  *   codes       [T][Kp] int8.    exponents  [T][Kp / G] bytes: e + 127; 0 a group of zeros; 255, over codes of 0, a
  *               group with a value that is not finite (or whose rotation is not), which comes back as NaN.
+ *               Both NULL: nothing is kept, as where no backward pass follows (not for DHQ_ACT_NONE); y has the same bits.
  *   y           [T][K] of `dtype`, leading dimension ldy; NULL for DHQ_ACT_NONE.  y may be x itself (same ldy).
  */
 DHQ_API dhq_status_t dhq_checkpoint_save(const void *x, dhq_dtype_t dtype, int64_t T, int64_t K, int64_t ldx, int group,

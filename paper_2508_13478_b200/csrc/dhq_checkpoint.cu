@@ -315,6 +315,10 @@ __global__ void __launch_bounds__(kThreads, kBlocksOf<MOVE>) save_kernel(const T
                     store8<T, true>(y + at.row * ldy + k, at.any ? K - k : 0, o[c]);
                 }
         }
+        if (ACT != DHQ_ACT_NONE && !codes) { // (no checkpoint)
+            if (MOVE == kDirect) break;
+            continue;
+        }
         if (ROT) rotate_span(v, G);
         float top[4];
 #pragma unroll
@@ -513,7 +517,8 @@ extern "C" dhq_status_t dhq_checkpoint_save(const void *x, dhq_dtype_t dtype, in
     if (s != DHQ_OK) return s;
     if (T == 0) return DHQ_OK;
     const bool with_y = activation != DHQ_ACT_NONE;
-    if (!good_matrix(x, K, ldx, dtype) || !codes || !aligned(codes, 16) || !exponents) return DHQ_ERR_INVALID_ARG;
+    const bool keep = codes || exponents; // (else y alone)
+    if (!good_matrix(x, K, ldx, dtype) || (keep ? !codes || !aligned(codes, 16) || !exponents : !with_y)) return DHQ_ERR_INVALID_ARG;
     if (with_y ? !good_matrix(y, K, ldy, dtype) : y != nullptr) return DHQ_ERR_INVALID_ARG;
     const int64_t Kp = padded_columns(K, group);
     const uint32_t spans = (uint32_t)((Kp + kSpan - 1) / kSpan);
@@ -530,7 +535,7 @@ extern "C" dhq_status_t dhq_checkpoint_save(const void *x, dhq_dtype_t dtype, in
                     auto go = [&](auto move) {
                         constexpr Move M = decltype(move)::value;
                         done = launch_spans(save_kernel<E, R, A, M>, M, kSaveSmem<E, M>, blocks, (cudaStream_t)stream, (const E *)x + first * ldx, ldx, rows, (int)K, (int)Kp,
-                                            group, spans, act, codes + first * Kp, exponents + first * (Kp / group), with_y ? (E *)y + first * ldy : (E *)nullptr, ldy);
+                                            group, spans, act, keep ? codes + first * Kp : nullptr, keep ? exponents + first * (Kp / group) : nullptr, with_y ? (E *)y + first * ldy : (E *)nullptr, ldy);
                     };
                     if (wide) go(std::integral_constant<Move, move_of<E>(true)>());
                     else go(std::integral_constant<Move, kRagged>());

@@ -177,7 +177,7 @@ def dhq_w4_linear(codes, scales, x, out, bias=None, group=128, rotation=DHQ_ROT_
 
 def dhq_checkpoint_save(x, codes, exponents, out=None, activation=DHQ_ACT_NONE, omega0=30.0, act_s0=0.0, group=128,
                         rotation=DHQ_ROT_NONE, stream=None):
-    """Checkpoint of x [T][K], and out = act(x) unless the activation is DHQ_ACT_NONE (out may be x)."""
+    """Checkpoint of x [T][K], and out = act(x) unless the activation is DHQ_ACT_NONE (out may be x).  codes and exponents None: out alone."""
     t, k, lead, device, address = _matrix(x, "x")
     padded = _padded(k, group)
     out_lead, out_address = 0, None
@@ -185,9 +185,11 @@ def dhq_checkpoint_save(x, codes, exponents, out=None, activation=DHQ_ACT_NONE, 
         out_lead, out_address = _result(out, "out", x.dtype, (t, k), device)
     elif activation != DHQ_ACT_NONE:
         raise TypeError("out: the activation's result needs a tensor")
+    kept = None, None
+    if codes is not None or exponents is not None:
+        kept = _store(codes, "codes", torch.int8, (t, padded), device), _store(exponents, "exponents", torch.uint8, (t, padded // group), device)
     code = _functions()["dhq_checkpoint_save"](
-        address, _TYPES[x.dtype], t, k, lead, group, rotation, activation, omega0, act_s0, _store(codes, "codes", torch.int8, (t, padded), device),
-        _store(exponents, "exponents", torch.uint8, (t, padded // group), device), out_address, out_lead, _stream_of(stream, device))
+        address, _TYPES[x.dtype], t, k, lead, group, rotation, activation, omega0, act_s0, *kept, out_address, out_lead, _stream_of(stream, device))
     if code:
         raise DhqError(code, "dhq_checkpoint_save")
 

@@ -7,6 +7,8 @@ linear layer need its weights only and are exact; weight gradients and slopes of
 Under torch.autocast a linear layer multiplies in autocast's type, forward and backward, as torch's own does; it keeps its input as it came, and
 the gradient of fp32 weights is summed and written in fp32.
 
+Where no backward pass can follow (gradients are off, or none is asked for) nothing is kept.
+
 A forward and backward pass may be captured into a CUDA graph in torch's way: warmed up on a side stream, with no eager graph of the same
 leaves alive when the capture begins (torch's gradient accumulation would wait for a stream that is not being captured).
 """
@@ -34,6 +36,11 @@ def _rows(t):
     return t if fits else t.clone(memory_format=torch.contiguous_format)
 
 
+def _product(x, x2, weight, bias):
+    y = x2 @ weight.t() if bias is None else torch.addmm(bias, x2, weight.t())
+    return y.reshape(*x.shape[:-1], weight.shape[0])
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
     @torch.amp.custom_fwd(device_type="cuda")
@@ -45,8 +52,7 @@ class _Linear(torch.autograd.Function):
             codes, exponents = _storage(x2.shape[0], x2.shape[1], group, x.device)
             dhq_checkpoint_save(x2, codes, exponents, activation=DHQ_ACT_NONE, group=group, rotation=rotation)
         ctx.save_for_backward(weight, codes, exponents)
-        y = x2 @ weight.t() if bias is None else torch.addmm(bias, x2, weight.t())
-        return y.reshape(*x.shape[:-1], weight.shape[0])
+        return _product(x, x2, weight, bias)
 
     @staticmethod
     @once_differentiable
@@ -65,16 +71,22 @@ class _Linear(torch.autograd.Function):
         return dx, dw, db, None, None
 
 
+def _activate(z, keep, form):
+    """act(z), and the checkpoint's codes and exponents (None unless they are kept)."""
+    z2 = _rows(z)
+    codes, exponents = _storage(z2.shape[0], z2.shape[1], form["group"], z.device) if keep else (None, None)
+    y = torch.empty(z2.shape, dtype=z.dtype, device=z.device)
+    dhq_checkpoint_save(z2, codes, exponents, out=y, **form)
+    return y.reshape(z.shape), codes, exponents
+
+
 class _Activation(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, z, activation, omega0, act_s0, group, rotation):
-        z2 = _rows(z)
-        codes, exponents = _storage(z2.shape[0], z2.shape[1], group, z.device)
-        y = torch.empty(z2.shape, dtype=z.dtype, device=z.device)
-        dhq_checkpoint_save(z2, codes, exponents, out=y, activation=activation, omega0=omega0, act_s0=act_s0, group=group, rotation=rotation)
+    def forward(ctx, z, form):
+        y, codes, exponents = _activate(z, True, form)
         ctx.save_for_backward(codes, exponents)
-        ctx.form = dict(activation=activation, omega0=omega0, act_s0=act_s0, group=group, rotation=rotation)
-        return y.reshape(z.shape)
+        ctx.form = form
+        return y
 
     @staticmethod
     @once_differentiable
@@ -83,14 +95,19 @@ class _Activation(torch.autograd.Function):
         dy2 = _rows(dy)
         dz = torch.empty(dy2.shape, dtype=dy.dtype, device=dy.device)
         dhq_checkpoint_act_grad(codes, exponents, dy2, dz, **ctx.form)
-        return dz.reshape(dy.shape), None, None, None, None, None
+        return dz.reshape(dy.shape), None
 
 
 def checkpointed_linear(x, weight, bias=None, group=64, rotation=DHQ_ROT_INPUT):
     """x weight^T + bias (fp32, bf16 or fp16 CUDA tensors, of one dtype unless autocast is on; x [..., K]), keeping x as an 8-bit checkpoint for the weight's gradient."""
+    if not torch.is_grad_enabled():   # (within a function of autograd it always is off)
+        return _product(x, _rows(x), weight, bias)
     return _Linear.apply(x, weight, bias, group, rotation)
 
 
 def checkpointed_activation(z, activation=DHQ_ACT_SINE, omega0=30.0, act_s0=0.0, group=64, rotation=DHQ_ROT_INPUT):
     """act(z), keeping z as an 8-bit checkpoint for the slope; activations as for dhq_checkpoint_save, but DHQ_ACT_NONE."""
-    return _Activation.apply(z, activation, omega0, act_s0, group, rotation)
+    form = dict(activation=activation, omega0=omega0, act_s0=act_s0, group=group, rotation=rotation)
+    if not (torch.is_grad_enabled() and z.requires_grad):
+        return _activate(z, False, form)[0]
+    return _Activation.apply(z, form)
