@@ -15,7 +15,8 @@ fp32 network's own output.
 
     python -m paper_2508_13478_b200.quality --size 256 --width 256 --hidden 3 --steps 3000
 
-With --checkpoints GROUP the fit keeps layer inputs and phases in 8 bits per value between forward and backward pass.
+With --checkpoints GROUP the fit keeps layer inputs and phases in 8 bits per value between forward and backward pass, rotated
+group by group unless --checkpoint-rotation none is given.
 """
 from __future__ import annotations
 
@@ -58,11 +59,12 @@ def ssim(a: np.ndarray, b: np.ndarray, peak: float = 1.0) -> float:
     return float(np.mean(vals))
 
 
-def fit_network(dims, omega0, target, coords, steps, lr, seed, gabor_s0=0.0, log=None, checkpoints=0):
+def fit_network(dims, omega0, target, coords, steps, lr, seed, gabor_s0=0.0, log=None, checkpoints=0, checkpoint_rotation=0):
     """Short fp32 fit of sin(omega0 (W x + b)) layers (or the Gabor wavelet) to `target` [n][d_L] in
     [-1, 1] by Adam on the mean squared error, from the seeded SIREN initialisation.  Returns the
     fitted (weights, biases) as fp32 numpy arrays and the network's own fp32 output.  checkpoints: 0, or
-    the group (32, 64, 128) of the 8-bit checkpoints that the backward pass works from."""
+    the group (32, 64, 128) of the 8-bit checkpoints that the backward pass works from; checkpoint_rotation:
+    DHQ_ROT_INPUT (0) or DHQ_ROT_NONE."""
     import torch
     import dhq_inputs
     from . import training
@@ -77,9 +79,10 @@ def fit_network(dims, omega0, target, coords, steps, lr, seed, gabor_s0=0.0, log
     def forward():
         x = x0
         for l in range(len(W)):
-            z = training.checkpointed_linear(x, W[l], B[l], checkpoints) if checkpoints else x @ W[l].T + B[l]
+            z = training.checkpointed_linear(x, W[l], B[l], checkpoints, checkpoint_rotation) if checkpoints else x @ W[l].T + B[l]
             if l < len(W) - 1 and checkpoints:
-                x = training.checkpointed_activation(z, training.DHQ_ACT_GABOR if gabor_s0 > 0 else training.DHQ_ACT_SINE, omega0, gabor_s0, checkpoints)
+                x = training.checkpointed_activation(z, training.DHQ_ACT_GABOR if gabor_s0 > 0 else training.DHQ_ACT_SINE, omega0, gabor_s0, checkpoints,
+                                                     checkpoint_rotation)
             elif l < len(W) - 1:
                 x = torch.sin(omega0 * z)
                 if gabor_s0 > 0:
@@ -173,17 +176,17 @@ def default_variants():
     return v
 
 
-def run(size=256, width=256, hidden=3, channels=1, steps=3000, lr=1e-4, omega0=30.0, seed=7, gabor_s0=0.0, log=None, checkpoints=0):
+def run(size=256, width=256, hidden=3, channels=1, steps=3000, lr=1e-4, omega0=30.0, seed=7, gabor_s0=0.0, log=None, checkpoints=0, checkpoint_rotation=0):
     import dhq_inputs
     dims = (2,) + (width,) * hidden + (channels,)
     image = dhq_inputs.procedural_image(size, size, channels, seed)
     coords = dhq_inputs.grid_coords(size, size)
     target = (image.reshape(-1, channels) * 2.0 - 1.0).astype(np.float32)
-    weights, biases, fp32_out = fit_network(dims, omega0, target, coords, steps, lr, seed, gabor_s0, log, checkpoints)
+    weights, biases, fp32_out = fit_network(dims, omega0, target, coords, steps, lr, seed, gabor_s0, log, checkpoints, checkpoint_rotation)
     shape = (size, size, channels)
     ref = to_image(fp32_out, shape)
     record = {"target": f"procedural image {size}x{size}x{channels}, seed {seed}", "dims": list(dims), "omega0": omega0,
-              "activation": "gabor" if gabor_s0 > 0 else "sine", "gabor_s0": gabor_s0, "fit": {"steps": steps, "lr": lr, "checkpoints": checkpoints},
+              "activation": "gabor" if gabor_s0 > 0 else "sine", "gabor_s0": gabor_s0, "fit": {"steps": steps, "lr": lr, "checkpoints": checkpoints, **({"checkpoint_rotation": checkpoint_rotation} if checkpoints else {})},
               "fp32_torch": {"psnr": psnr(ref, image), "ssim": ssim(ref, image)}, "variants": {}}
     for name, out in evaluate(dims, omega0, weights, biases, coords, default_variants(), gabor_s0).items():
         img = to_image(out, shape)
@@ -193,6 +196,7 @@ def run(size=256, width=256, hidden=3, channels=1, steps=3000, lr=1e-4, omega0=3
 
 
 def main():
+    from . import binding
     ap = argparse.ArgumentParser()
     ap.add_argument("--size", type=int, default=256)
     ap.add_argument("--width", type=int, default=256)
@@ -204,9 +208,11 @@ def main():
     ap.add_argument("--seed", type=int, default=7)
     ap.add_argument("--gabor-s0", type=float, default=0.0, help="> 0: the wavelet activation (WIRE reading) instead of the sine")
     ap.add_argument("--checkpoints", type=int, default=0, choices=(0, 32, 64, 128), help="group of 8-bit checkpoints for the fit; 0: none")
+    ap.add_argument("--checkpoint-rotation", choices=("input", "none"), default="input", help="rotation of the checkpoints' groups")
     args = ap.parse_args()
     rec = run(args.size, args.width, args.hidden, args.channels, args.steps, args.lr, args.omega0, args.seed, args.gabor_s0,
-              log=lambda m: print(m, file=sys.stderr), checkpoints=args.checkpoints)
+              log=lambda m: print(m, file=sys.stderr), checkpoints=args.checkpoints,
+              checkpoint_rotation={"input": binding.DHQ_ROT_INPUT, "none": binding.DHQ_ROT_NONE}[args.checkpoint_rotation])
     print(json.dumps(rec))
 
 
