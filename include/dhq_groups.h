@@ -95,7 +95,8 @@ DHQ_API dhq_status_t dhq_checkpoint_act_grad(const int8_t *codes, const uint8_t 
 
 /*
  * Weight gradient of a linear layer y = x W^T (+ b) whose input x was kept as a checkpoint: dW = dy^T x^, the sum over the
- * T rows.  T = 0 writes zeros.  Every sum is taken in the same order in every call with the same sizes and types.
+ * T rows.  T = 0 writes zeros.  (A wait inside the kernel for copies or products of its own that lasts two seconds, which no sound GPU has, ends that block with NaN
+ * in its part of dW; the call has returned OK by then.)  Every sum is taken in the same order in every call with the same sizes and types.
  *   dy         [T][N] of `dtype`, leading dimension lddy.
  *   dW         [N][K] of `dw_dtype` (DHQ_F32, or the type of dy), leading dimension lddw; overwritten.
  *   workspace  device, `workspace_bytes` of at least what dhq_checkpoint_weight_grad_workspace says for the same

@@ -32,6 +32,7 @@
 #include "dhq_group.cuh"
 #include "dhq_tmem.cuh"
 #include "dhq_internal.cuh"
+#include "dhq_wait.h"
 #include <algorithm>
 #include <cuda.h>
 
@@ -44,7 +45,7 @@ constexpr int kLoadWarps = 16, kLoadTurns = 2; // fp32 dy: a half of the warps t
 template <class T> constexpr int kChunkOf = std::is_same<T, __half>::value ? 8 : 16;
 constexpr int kScaleWords = 272; // of a stage: pairs of powers [4 groups][32 pairs of rows], the same for tiny fp16 groups, whether there are any
 constexpr int kPitch = kTileK + 4; // floats of a row of the finished tile in shared memory: two rows of a quarter warp meet no bank twice
-constexpr unsigned long long kWaitLimit = 2000000000ull; // ns: a wait that long ends the kernel, with NaN for results
+constexpr unsigned long long kWaitLimit = 2000000000ull; // ns: a wait that long ends the block, with NaN for results
 
 // B operand in shared memory: MN-major, 128-byte swizzle.  64 features (128 bytes) x 64 rows make a box of 8 KB, boxes follow one another.
 __device__ __forceinline__ uint64_t desc_mn(uint32_t addr)
@@ -130,14 +131,9 @@ constexpr int kGradSmem = kRingBytes<T, BN, DRAIN> + kStagesB<T, BN, DRAIN> * kS
 
 struct Waiter {
     volatile int *failed;
-    unsigned long long begun;
     __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const
     {
-        while (!ptx::mbar_try_wait_hint(bar, parity, 20000)) {
-            if (*failed) return false;
-            if (ptx::globaltimer() - begun > kWaitLimit) *failed = 1;
-        }
-        return true;
+        return wait_bounded([&] { return ptx::mbar_try_wait_hint(bar, parity, 20000); }, [] { return ptx::globaltimer(); }, kWaitLimit, failed);
     }
 };
 
@@ -300,7 +296,7 @@ weight_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ C
     ptx::tc_fence_after();
     ptx::launch_dependents();
     const uint32_t tmem = ptx::uniform(tmem_holder), first_a = tmem + kFirstA<T, BN, DRAIN>;
-    const Waiter wait{&failed, ptx::globaltimer()};
+    const Waiter wait{&failed};
 
     // The whole tile; the second time with powers of e - s and the groups' shifts s, a byte each.
     auto take_tile = [&](auto again, uint32_t shifts) {
