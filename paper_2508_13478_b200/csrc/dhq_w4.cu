@@ -597,7 +597,7 @@ LinearPlan plan_of(int64_t T, int64_t N, int64_t K, int group, bool rot, dhq_dty
         p.per_rank = (p.blocks + p.ranks - 1) / p.ranks;
         p.smem = size(2, part_blocks(p.nt), 8 * p.nt, kWarps);
         p.term_bytes = (int64_t)p.token_blocks * 8 * p.nt * p.blocks * kBlockK * 2;
-        p.factor_bytes = p.token_blocks * p.blocks * groups * 8 * p.nt * 8;
+        p.factor_bytes = (int64_t)p.token_blocks * p.blocks * groups * 8 * p.nt * 8;
     }
     return p;
 }
