@@ -105,7 +105,7 @@ DHQ_API dhq_status_t dhq_checkpoint_act_grad(const int8_t *codes, const uint8_t 
  *              run at the same time need one each.
  * fp16 dy: the q 2^e of a group are fp16 numbers times a power of two, which is one for the rows that a block sums and such that the largest is
  * finite (1 while q 2^e stay below 65,504, and then nothing of them is rounded; else what lies 2^39 below the largest is).
- * Errors: also ALLOC if the workspace is too small.
+ * Errors: also ALLOC if the workspace is too small, UNSUPPORTED for sizes that make more blocks than a launch has (far beyond any memory).
  */
 DHQ_API dhq_status_t dhq_checkpoint_weight_grad_workspace(int64_t T, int64_t N, int64_t K, int group, dhq_rot_t rotation,
                                                           dhq_dtype_t dtype, const void *dy, int64_t lddy,

@@ -732,7 +732,9 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ GradA
 
 struct GradPlan {
     int bn, k_tiles, n_tiles, splits, steps;
+    int64_t blocks, join_blocks; // of the two launches
     int64_t part_bytes, copy_bytes, copy_ld; // of the workspace; elements of a row of the copy
+    bool launchable() const { return std::max(blocks, join_blocks) < (int64_t)1 << 31; }
 };
 // BN = 128 where 256 would leave half of every tile empty, for fp32 dy (three terms, two sets of sums), and for fp32 sums that
 // are drained (running sums of 128 x 256 would leave the ring two stages: 527 us for 8,192 rows, 4,096 x 4,096; now 370).  Rows are split where tiles alone do not
@@ -758,7 +760,9 @@ GradPlan plan_of(int64_t T, int64_t N, int64_t K, int group, dhq_dtype_t dtype, 
         const double t = rounds * (step * ((p.steps + s - 1) / s) + 4.0) + (s > 1 ? 4.0 + 8.0 * s * tiles * p.bn * kTileK / 4e6 : 0.0);
         if (t < best) best = t, p.splits = s;
     }
-    p.part_bytes = p.splits > 1 ? p.splits * tiles * p.bn * kTileK * 4 : 0;
+    p.blocks = tiles * p.splits;
+    p.join_blocks = p.splits > 1 ? tiles * (p.bn / (p.splits >= 8 ? 8 : 64)) : 0;
+    p.part_bytes = p.splits > 1 && p.launchable() ? p.splits * tiles * p.bn * kTileK * 4 : 0;
     p.copy_ld = (N + 7) / 8 * 8;
     p.copy_bytes = dtype != DHQ_F32 && !aligned_rows ? T * p.copy_ld * 2 : 0;
     return p;
@@ -827,6 +831,7 @@ extern "C" dhq_status_t dhq_checkpoint_weight_grad_workspace(int64_t T, int64_t 
     if (s != DHQ_OK) return s;
     if (dw_dtype != DHQ_F32 && dw_dtype != dtype) return DHQ_ERR_INVALID_ARG;
     const GradPlan p = plan_of(T, N, K, group, dtype, dw_dtype, rows_of_16(dy, lddy, dtype));
+    if (!p.launchable()) return DHQ_ERR_UNSUPPORTED;
     *bytes = p.part_bytes + p.copy_bytes;
     return DHQ_OK;
 }
@@ -842,6 +847,7 @@ extern "C" dhq_status_t dhq_checkpoint_weight_grad(const int8_t *codes, const ui
     if (!good_matrix(dW, K, lddw, dw_dtype)) return DHQ_ERR_INVALID_ARG;
     if (T > 0 && (!codes || !aligned(codes, 16) || !exponents || !good_matrix(dy, N, lddy, dtype))) return DHQ_ERR_INVALID_ARG;
     const GradPlan p = plan_of(T, N, K, group, dtype, dw_dtype, rows_of_16(dy, lddy, dtype));
+    if (!p.launchable()) return DHQ_ERR_UNSUPPORTED;
     const int64_t need = p.part_bytes + p.copy_bytes;
     if (need && (!workspace || !aligned(workspace, 16))) return DHQ_ERR_INVALID_ARG;
     if (workspace_bytes < need) return DHQ_ERR_ALLOC;

@@ -20,3 +20,14 @@ def test_workspace_of_products_of_any_size(t, n, k, group, kind, rotation):
     need = C.c_int64(-1)
     assert groups._functions()["dhq_w4_linear_workspace"](t, n, k, group, rotation, kind, C.byref(need)) == 0
     assert need.value == columns * blocks * 256 * 2 + columns * blocks * (256 // group) * 8
+
+
+def test_weight_gradients_of_more_blocks_than_a_launch_has():
+    need = C.c_int64(-1)
+    ask = groups._functions()["dhq_checkpoint_weight_grad_workspace"]
+    rows = (1 << 31) - 1
+    for t, n, k, kind, out in ((rows, 1 << 20, 1 << 20, 2, 2), (rows, 1 << 14, 1 << 24, 2, 2), (rows, 1 << 24, 1 << 18, 1, 1)):
+        assert ask(t, n, k, 64, dhq.DHQ_ROT_NONE, kind, 1 << 20, n, out, C.byref(need)) == 2, (t, n, k)
+    # the most rows, for one tile: a part of it (128 x 128 sums) for every 16,384 of fp16
+    assert ask(rows, 64, 64, 64, dhq.DHQ_ROT_NONE, 2, 1 << 20, 64, 2, C.byref(need)) == 0 and need.value == (1 << 17) * 128 * 128 * 4
+    assert ask(8192, 8192, 8192, 128, dhq.DHQ_ROT_INPUT, 1, 1 << 20, 8192, 1, C.byref(need)) == 0
