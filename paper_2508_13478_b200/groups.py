@@ -9,6 +9,7 @@ these four are contiguous.
 from __future__ import annotations
 
 import ctypes
+from functools import lru_cache
 
 import torch
 
@@ -150,9 +151,14 @@ def dhq_w4_pack(weight, codes, scales, group=128, rotation=DHQ_ROT_NONE, stream=
         raise DhqError(code, "dhq_w4_pack")
 
 
+@lru_cache(maxsize=1024)   # (sizes and types alone decide; a call of a few microseconds of device time asks each time)
+def _linear_need(*sizes):
+    return _need("dhq_w4_linear_workspace", *sizes)
+
+
 def dhq_w4_linear_workspace(t, n, k, dtype, group=128, rotation=DHQ_ROT_NONE) -> int:
     """Bytes that dhq_w4_linear needs beside its arguments."""
-    return _need("dhq_w4_linear_workspace", t, n, k, group, rotation, _TYPES[dtype])
+    return _linear_need(t, n, k, group, rotation, _TYPES[dtype])
 
 
 def dhq_w4_linear(codes, scales, x, out, bias=None, group=128, rotation=DHQ_ROT_NONE, workspace=None, stream=None):
@@ -164,9 +170,7 @@ def dhq_w4_linear(codes, scales, x, out, bias=None, group=128, rotation=DHQ_ROT_
     out_lead, out_address = _result(out, "out", dtype, (t, n), device)
     padded = _padded(k, group)
     raw = _stream_of(stream, device)
-    where, size, keep = None, 0, None
-    if t > 2 or k > 4096 or workspace is not None:   # (otherwise it is 0)
-        where, size, keep = _workspace(workspace, dhq_w4_linear_workspace(t, n, k, dtype, group, rotation), device, stream)
+    where, size, _keep = _workspace(workspace, _linear_need(t, n, k, group, rotation, _TYPES[dtype]), device, stream)
     code = _functions()["dhq_w4_linear"](
         _store(codes, "codes", torch.uint8, (n, padded // 2), device), _store(scales, "scales", torch.bfloat16, (n, padded // group), device), n, k,
         group, rotation, address, _TYPES[dtype], t, lead, None if bias is None else _store(bias, "bias", dtype, (n,), device),

@@ -31,3 +31,31 @@ def test_weight_gradients_of_more_blocks_than_a_launch_has():
     # the most rows, for one tile: a part of it (128 x 128 sums) for every 16,384 of fp16
     assert ask(rows, 64, 64, 64, dhq.DHQ_ROT_NONE, 2, 1 << 20, 64, 2, C.byref(need)) == 0 and need.value == (1 << 17) * 128 * 128 * 4
     assert ask(8192, 8192, 8192, 128, dhq.DHQ_ROT_INPUT, 1, 1 << 20, 8192, 1, C.byref(need)) == 0
+
+
+def test_the_binding_asks_the_library_for_every_size(monkeypatch):
+    """No rule of the library's is repeated in Python: what dhq_w4_linear_workspace says is what the call gets."""
+    torch = pytest.importorskip("torch")
+    seen = []
+
+    def need(name, t, n, k, group, rotation, kind):
+        seen.append((name, t, k))
+        return 0
+
+    class Stop(Exception):
+        pass
+
+    def stop(*_):
+        raise Stop
+
+    monkeypatch.setattr(groups, "_need", need)
+    if hasattr(groups, "_linear_need"):   # (answers of this test's own are not remembered)
+        monkeypatch.setattr(groups, "_linear_need", lambda *sizes: need("dhq_w4_linear_workspace", *sizes))
+    monkeypatch.setattr(groups, "_matrix", lambda t, what: (*t.shape, t.shape[1], 0, 1 << 20))
+    monkeypatch.setattr(groups, "_result", lambda t, *_: (t.shape[1], 1 << 20))
+    monkeypatch.setattr(groups, "_stream_of", lambda *_: None)
+    monkeypatch.setattr(groups, "_store", stop)
+    for t, k in ((1, 64), (2, 4000), (3, 64), (1, 9000)):
+        with pytest.raises(Stop):
+            groups.dhq_w4_linear(None, None, torch.zeros(t, k), torch.zeros(t, 24), group=32)
+        assert seen[-1][1:] == (t, k)
