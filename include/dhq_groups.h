@@ -50,9 +50,11 @@ DHQ_API dhq_status_t dhq_w4_pack(const void *W, dhq_dtype_t dtype, int64_t N, in
  * the codes are read once for every 64 columns (rows times terms, see below).
  * Accuracy: products are summed in fp32 on the tensor cores, with one multiply by the scale per group and one rounding to the type
  * of `out`.  x~ goes there as fp16 numbers times a power of two per row and group: 16-bit x as one, exactly (below 2^-28 of its
- * group's largest value it may lose bits), rotated bf16 x as one (2^-12 of a value; the result is rounded to 2^-9), fp32 and rotated fp16 x as
- * two terms (2^-24).  A row of x with values that are not finite has no finite results (with 16-bit x they may all be NaN); other rows
- * are not touched by it.  Range: 16-bit x wants scales below 2^103 and magnitudes of x~ from 2^-126 on.
+ * group's largest value it may lose bits), rotated bf16 x as one (off by 2^-11 of a value at most; the result is rounded by up to 2^-8), fp32 and
+ * rotated fp16 x as two terms (2^-23).  With 16-bit x a group's sum is formed as sum (q + 8) x~ - 8 sum x~: what fp32 rounds is relative
+ * to the larger one of these, which costs up to 5 of its 24 bits where x~ has one sign.  A row of x with values that are not finite has no finite results
+ * (with 16-bit x they may all be NaN); other rows are not touched by it.  Range: 16-bit x wants scales below 2^103 and magnitudes of x~ from 2^-126 on,
+ * fp32 x 7 G max |x~| below 2^128 (sums of codes times values are taken before the scale).
  *   x     [T][K] of `dtype`, leading dimension ldx.     bias  [N] of `dtype`, or NULL.
  *   out   [T][N] of `dtype`, leading dimension ldout.
  *   workspace  device, `workspace_bytes` of at least what dhq_w4_linear_workspace says, 16-byte aligned; NULL where that is 0
@@ -74,8 +76,12 @@ DHQ_API dhq_status_t dhq_w4_linear(const uint8_t *codes, const uint16_t *scales,
  * products of dhq_checkpoint_weight_grad round nothing of it.  1 + 1/G bytes per value.
  *   x           [T][K] of `dtype`, leading dimension ldx.
  *   activation  DHQ_ACT_NONE (x is the input of a linear layer: no y), DHQ_ACT_SINE sin(omega0 x), DHQ_ACT_GABOR
- *               sin(omega0 x) exp(-(act_s0 x)^2), DHQ_ACT_SILU x / (1 + exp(-x)), DHQ_ACT_GELU x Phi(x) (with erf).
+ *               sin(omega0 x) exp(-(act_s0 x)^2), DHQ_ACT_SILU x / (1 + exp(-x)), DHQ_ACT_GELU x Phi(x) (Phi the normal
+ *               distribution's, not the approximation with tanh).
  *               omega0 and act_s0 (finite; act_s0 > 0 for the wavelet) are ignored by the others.
+ *               Accuracy of fp32 results, before the rounding to `dtype`: 2^-19 for the sine and the wavelet, with phases below 2^22 turns (beyond, sines
+ *               of some phase; NaN where |omega0 x| / 2 pi is more than fp32 holds), 2^-19 |x| for the others.  These are bounds; root mean squares are 1.1e-7,
+ *               and 6e-8 for silu and 1e-7 for gelu of x with a standard deviation of 2.
  *   codes       [T][Kp] int8.    exponents  [T][Kp / G] bytes: e + 127; 0 a group of zeros; 255, over codes of 0, a
  *               group with a value that is not finite (or whose rotation is not), which comes back as NaN.
  *               Both NULL: nothing is kept, as where no backward pass follows (not for DHQ_ACT_NONE); y has the same bits.
@@ -87,6 +93,8 @@ DHQ_API dhq_status_t dhq_checkpoint_save(const void *x, dhq_dtype_t dtype, int64
 
 /*
  * Backward pass of that activation from the checkpoint: dx = dy act'(x^).  DHQ_ACT_NONE is UNSUPPORTED (dx = dy).
+ * Accuracy of act'(x^): 2^-19 of omega0 for the sine (phases as above), of omega0 + 2 act_s0 for the wavelet (NaN where 2 act_s0^2 x^ is more than fp32 holds), of 2 for
+ * the others.
  *   dy, dx  [T][K] of `dtype`, leading dimensions lddy, lddx.  dx may be dy itself (same leading dimension).
  */
 DHQ_API dhq_status_t dhq_checkpoint_act_grad(const int8_t *codes, const uint8_t *exponents, int64_t T, int64_t K, int group,
@@ -105,6 +113,9 @@ DHQ_API dhq_status_t dhq_checkpoint_act_grad(const int8_t *codes, const uint8_t 
  *              run at the same time need one each.
  * fp16 dy: the q 2^e of a group are fp16 numbers times a power of two, which is one for the rows that a block sums and such that the largest is
  * finite (1 while q 2^e stay below 65,504, and then nothing of them is rounded; else what lies 2^39 below the largest is).
+ * Accuracy: products are exact and summed on the tensor cores, which cut off what does not fit an fp32 sum.  fp32 results take the sums of at most
+ * 1,024 rows (512 of fp16 dy) from there and add these in fp32; for 16-bit results up to 65,536 rows of bf16 or 16,384 of fp16 stay there, by which a
+ * sum of one sign is too small by some 5e-5 of itself (measured).  Range: |q 2^e| below 2^127; sums of dy times rotated values are taken before H_G / G.
  * Errors: also ALLOC if the workspace is too small, UNSUPPORTED for sizes that make more blocks than a launch has (far beyond any memory).
  */
 DHQ_API dhq_status_t dhq_checkpoint_weight_grad_workspace(int64_t T, int64_t N, int64_t K, int group, dhq_rot_t rotation,

@@ -89,8 +89,10 @@ __global__ void __launch_bounds__(kPackThreads) pack_kernel(const T *W, int64_t 
 // offset by an exact fp16 addition per pair instead.
 //
 // x as fp16 numbers.  With 2^e the power of two that puts the largest magnitude of a group of x~ into [2^14, 2^15), x~ 2^e = hi + lo with hi
-// and lo fp16.  16-bit x is hi itself (values below 2^-28 of their group's largest may lose bits).  Rotated bf16 x is taken as hi, off by 2^-12 of a value,
-// its result is rounded to 2^-9.  fp32 and rotated fp16 x take both, off by 2^-24 as fp32 is.  lo makes further columns; the power
+// and lo fp16.  16-bit x is hi itself (values below 2^-28 of their group's largest may lose bits).  Rotated bf16 x is taken as hi, off by
+// at most 2^-11 of a value, where its result is rounded by up to 2^-8 (16 rows, 32,768 x 8,192: off by 1.667e-3 of the result's norm in all, a correctly rounded one
+// by 1.654e-3; both terms would make twice the columns, 56 -> 89 us).  fp32 and rotated fp16 x take both: lo holds 11 of the rest's bits, so they are off by
+// at most 2^-23.  lo makes further columns; the power
 // multiplies the finished sum of a group with the weights' scale, in fp32.
 //
 // Work of a block of 8 warps: 16 WR rows, WK = 8 / WR warps side by side along k.  Where the rows make too few blocks for the GPU
@@ -142,7 +144,8 @@ __device__ __forceinline__ uint4 load_shared16(uint32_t at)
 // A word of eight codes as four pairs of fp16 numbers: exactly the codes, or (the first and third) u 2^-24, (the others) 16 u 2^-24.
 template <bool EXACT> __device__ __forceinline__ void numbers(uint32_t w, uint32_t (&p)[4])
 {
-    // 0x6400 is 1024: a nibble in the lowest four bits of the mantissa adds itself, in the next four sixteen times itself
+    // 0x6400 is 1024: a nibble in the lowest four bits of the mantissa adds itself, in the next four sixteen times itself (integers to floating point by
+    // masks and one addition: Kim, Henry, Fahim, Awadalla, "Who Says Elephants Can't Run", 2022)
     const __half2 low = __float2half2_rn(-1032.0f), high = __float2half2_rn(-72.0f), sixteenth = __float2half2_rn(0.0625f);
 #pragma unroll
     for (int i = 0; i < 4; i += 2) {

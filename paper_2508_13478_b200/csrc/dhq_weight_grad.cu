@@ -8,8 +8,8 @@
 // fp16 holds 65,504 at most, and q 2^e of a rotated group is up to G times as large as its x (rounded, it is larger without the rotation, too: 64 2^10 for
 // 65,504).  A block whose dy is fp16 therefore takes its tile a second time if it has met such numbers: for each group with the least s at which
 // 127 2^(e - s) is finite, powers of e - s, and finished sums times 2^s.  Then what lies 2^39 below the group's largest is rounded.
-// The warp that makes powers of the exponents sees them anyway.  (8,192 rows, 4,096 x 4,096, groups of 128 / 32: 236 / 240 us without any of this, 242 / 248 with it,
-// for the second copy of the code beside the first; 253 / 277 where all warps look over the exponents first; as a function behind a call 245 / 265.)
+// The warp that makes powers of the exponents sees them anyway.  (8,192 rows, 4,096 x 4,096, groups of 128 / 32: 236 / 240 us without any of this, 237 / 243 with it;
+// 253 / 277 where all warps look over the exponents first, 243 / 252 with the second time as a copy of the code, 245 / 265 as a function behind a call.)
 //
 // What bounds it is the traffic of shared memory (128 bytes per cycle and SM), not only the tensor pipe: with both operands there a
 // 128 x 256 tile needs 96 bytes per cycle for the MMAs alone.  So x^ is the operand that lives in tensor memory (lane = input feature,
@@ -17,7 +17,8 @@
 // pairs of bytes (ldmatrix, free of bank conflicts under the 128-byte swizzle: a pair of inputs at two rows ends up in one register), make each
 // input's two rows 16-bit numbers in four instructions and store them with tcgen05.st, whose 16x128b form has just that layout.  dy is used as
 // it lies in global memory (rows of the batch outside, features inside: MN-major, 128-byte swizzle), by TMA.  8,192 rows, 8,192 x 8,192, bf16:
-// 896 us, 1,228 TFLOP/s, 0.88 of what cuBLAS sustains on a plain product; a step moves 84 KB through shared memory, 656 of its 730 cycles.
+// 896 us at full clock, 1,228 TFLOP/s, 0.73 of a plain product by cuBLAS in a short burst (in a loop of seconds, under the power limit, 1,043 to 1,074 us, 0.74 to 0.76 of
+// cuBLAS there); a step moves 84 KB through shared memory, 656 of its 730 cycles.
 // (Codes read from global memory by the converting warps, 8 rows x 32 bytes a load: 1,109 us; transposed in registers, movmatrix: 930.)
 //
 // Sums.  The tensor cores cut off what does not fit a sum, so that a sum of n products of 16 is too small by some 2e-8 n / 4 of itself: 3e-7
@@ -119,7 +120,8 @@ template <class T> constexpr int kThreadsOf = 32 * (kConvertWarpsOf<T> + (std::i
 // 32 columns.
 template <class T, int BN, bool DRAIN> constexpr int kFirstA = (std::is_same<T, float>::value ? 3 : DRAIN ? 2 : 1) * BN;
 template <class T, int BN, bool DRAIN> constexpr int kStagesA = std::is_same<T, float>::value || (BN == 128 && !DRAIN) ? 4 : 8;
-// Shared memory: ring of dy and codes, powers, running sums.  (BN = 128 without running sums: two blocks to an SM.  A ring of codes that runs two
+// Shared memory: ring of dy and codes, powers, running sums.  (BN = 128 without running sums is sized for two blocks to an SM, but 19 warps of
+// 80 registers a thread leave room for one.  A ring of codes that runs two
 // steps ahead of dy's: 936 us for 8,192 rows, 8,192 x 8,192, against 905.)
 template <class T, int BN> constexpr int kDyBytes = BN * kStep * 2 * kTermsOf<T>;
 template <class T, int BN> constexpr int kStageBytes = kDyBytes<T, BN> + kTileK * kStep;
@@ -298,9 +300,8 @@ weight_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ C
     const uint32_t tmem = ptx::uniform(tmem_holder), first_a = tmem + kFirstA<T, BN, DRAIN>;
     const Waiter wait{&failed};
 
-    // The whole tile; the second time with powers of e - s and the groups' shifts s, a byte each.
-    auto take_tile = [&](auto again, uint32_t shifts) {
-        constexpr bool AGAIN = decltype(again)::value;
+    uint32_t shifts = 0; // HALF: s of each group, a byte each
+    for (;;) {
         if (warp < CW) {
             // x^: inputs 32 * (warp % 4) on of the tile, all rows of a step
             const int quarter = warp & 3, turn = warp >> 2;
@@ -394,7 +395,7 @@ weight_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ C
             ptx::tc_fence_after();
             converters_sync<CW>(); // everyone is past the ring
             const int64_t out = a.partial ? (int64_t)blockIdx.x * BN * kTileK : 0;
-            const float up = AGAIN ? power_of(127u + (shifts >> (8 * (x / a.G)) & 255u)) : 1.0f;
+            const float up = HALF ? power_of(127u + (shifts >> (8 * (x / a.G)) & 255u)) : 1.0f;
 #pragma unroll 1
             for (int n = part; n < part + PART; n += 32) {
                 uint32_t v[32], w[32];
@@ -406,7 +407,7 @@ weight_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ C
                     float f = __uint_as_float(v[i]);
                     if (F32) f = __fadd_rn(f, __uint_as_float(w[i]));
                     if (drains > 0) f = __fadd_rn(running[(n + i) * kPitch + x], f);
-                    if (AGAIN) f = __fmul_rn(f, up);
+                    if (HALF) f = __fmul_rn(f, up);
                     f = steps == 0 ? 0.0f : ok && !failed ? f : __uint_as_float(0x7fffffffu);
                     if (a.partial) a.partial[out + (n + i) * kTileK + x] = f;
                     else running[(n + i) * kPitch + x] = f;
@@ -496,7 +497,7 @@ weight_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ C
                             byte[u][r] = 0;
 #pragma unroll
                             for (int g = 0; g < LOADS; ++g) byte[u][r] |= (uint32_t)e[u][r][g] << (8 * g);
-                            if (AGAIN) byte[u][r] = shifted(byte[u][r], shifts);
+                            if (HALF && shifts) byte[u][r] = shifted(byte[u][r], shifts);
                             if ((i0 + u) * kStep + 2 * lane + r >= rows) byte[u][r] = 0;
                         }
 #pragma unroll
@@ -510,7 +511,7 @@ weight_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ C
 #pragma unroll
                         for (int g = 0; g < COUNT; ++g) {
                             const uint32_t bytes = __byte_perm(byte[u][0], byte[u][1], 0x0400 + 0x0101 * g) & 0x00ff00ffu;
-                            if (HALF && !AGAIN) seen = __vmaxu2(seen, bytes);
+                            if (HALF) seen = __vmaxu2(seen, bytes);
                             pair[g] = powers16(bytes, small, M());
                         }
                         if (HALF) small = __any_sync(0xffffffffu, small);
@@ -533,7 +534,7 @@ weight_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ C
                         if (++s == SB) s = 0, round ^= 1;
                     }
                 }
-                if (HALF && !AGAIN && max(seen & 0xffffu, seen >> 16) > kLargestByte) large = 1;
+                if (HALF && max(seen & 0xffffu, seen >> 16) > kLargestByte) large = 1;
             };
             using std::integral_constant;
             const bool together = per_row % per_tile == 0 && ((uintptr_t)a.exponents & (per_tile - 1)) == 0;
@@ -614,40 +615,36 @@ weight_grad_kernel(const __grid_constant__ GradArgs a, const __grid_constant__ C
         }
         if (failed) __nanosleep(1000000); // copies and MMAs in flight end by themselves
         __syncthreads();
-    };
-    take_tile(std::false_type(), 0u);
-    if constexpr (HALF)
-        if (__builtin_expect(large, 0)) {
-            const int per_row = a.Kp / a.G, first = k0 / a.G, groups = min(kTileK / a.G, per_row - first);
-            const int64_t end = min((int64_t)(step0 + steps) * kStep, a.T);
-            for (int g = 0; g < groups; ++g) {
-                uint32_t top = 0;
-                for (int64_t r = (int64_t)step0 * kStep + threadIdx.x; r < end; r += kThreadsOf<T>) {
-                    const uint32_t byte = a.exponents[r * per_row + first + g];
-                    top = max(top, byte == 255u ? 0u : byte);
-                }
-                atomicMax(tops + g, top);
+        if (!HALF || shifts || !large) break;
+        const int per_row = a.Kp / a.G, first = k0 / a.G, groups = min(kTileK / a.G, per_row - first);
+        const int64_t end = min((int64_t)(step0 + steps) * kStep, a.T);
+        for (int g = 0; g < groups; ++g) {
+            uint32_t top = 0;
+            for (int64_t r = (int64_t)step0 * kStep + threadIdx.x; r < end; r += kThreadsOf<T>) {
+                const uint32_t byte = a.exponents[r * per_row + first + g];
+                top = max(top, byte == 255u ? 0u : byte);
             }
-            // Barriers and sums as at the beginning.  All copies, MMAs and drains have been waited for; the arrivals that say that stages are empty
-            // are, now.
-            if (warp == MMA_WARP) {
-                for (int s = 0; s < min(SB, steps); ++s) wait(empty_b(s), ((steps - 1 - s) / SB) & 1);
-                for (int s = 0; s < min(SA, steps); ++s) wait(empty_a(s), ((steps - 1 - s) / SA) & 1);
-            }
-            ptx::fence_proxy_async(); // (finished rows were written where copies go)
-            ptx::tc_fence_before();
-            __syncthreads();
-            uint32_t shifts = 0;
-            for (int g = 0; g < groups; ++g) shifts |= (max(tops[g], kLargestByte) - kLargestByte) << (8 * g);
-            if (threadIdx.x == 0) {
-                for (int i = 0; i < 3 * SB + 2 * SA + 5; ++i) mbar_inval(ptx::smem_u32(bars + i));
-                init_barriers();
-            }
-            const bool again = shifts && !failed; // (without shifts there are broken groups only)
-            __syncthreads();
-            ptx::tc_fence_after();
-            if (again) take_tile(std::true_type(), shifts);
+            atomicMax(tops + g, top);
         }
+        // Barriers and sums as at the beginning.  All copies, MMAs and drains have been waited for; the arrivals that say that stages are empty
+        // are, now.
+        if (warp == MMA_WARP) {
+            for (int s = 0; s < min(SB, steps); ++s) wait(empty_b(s), ((steps - 1 - s) / SB) & 1);
+            for (int s = 0; s < min(SA, steps); ++s) wait(empty_a(s), ((steps - 1 - s) / SA) & 1);
+        }
+        ptx::fence_proxy_async(); // (finished rows were written where copies go)
+        ptx::tc_fence_before();
+        __syncthreads();
+        for (int g = 0; g < groups; ++g) shifts |= (max(tops[g], kLargestByte) - kLargestByte) << (8 * g);
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < 3 * SB + 2 * SA + 5; ++i) mbar_inval(ptx::smem_u32(bars + i));
+            init_barriers();
+        }
+        const bool again = shifts && !failed; // (without shifts there are broken groups only)
+        __syncthreads();
+        ptx::tc_fence_after();
+        if (!again) break;
+    }
     if (warp == MMA_WARP) {
         ptx::tc_fence_after();
         ptx::tmem_dealloc(tmem, COLUMNS);
