@@ -17,7 +17,7 @@
 // pairs of bytes (ldmatrix, free of bank conflicts under the 128-byte swizzle: a pair of inputs at two rows ends up in one register), make each
 // input's two rows 16-bit numbers in four instructions and store them with tcgen05.st, whose 16x128b form has just that layout.  dy is used as
 // it lies in global memory (rows of the batch outside, features inside: MN-major, 128-byte swizzle), by TMA.  8,192 rows, 8,192 x 8,192, bf16:
-// 896 us at full clock, 1,228 TFLOP/s, 0.73 of a plain product by cuBLAS in a short burst (in a loop of seconds, under the power limit, 1,043 to 1,074 us, 0.74 to 0.76 of
+// 896 to 927 us at full clock, 1,186 to 1,228 TFLOP/s, 0.71 to 0.73 of a plain product by cuBLAS in a short burst (in a loop of seconds, under the power limit, 1,043 to 1,074 us, 0.74 to 0.76 of
 // cuBLAS there); a step moves 84 KB through shared memory, 656 of its 730 cycles.
 // (Codes read from global memory by the converting warps, 8 rows x 32 bytes a load: 1,109 us; transposed in registers, movmatrix: 930.)
 //
