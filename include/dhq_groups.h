@@ -112,7 +112,7 @@ DHQ_API dhq_status_t dhq_checkpoint_act_grad(const int8_t *codes, const uint8_t 
  *              aligned to 16 bytes.)  Used until the call's work on `stream` is done: calls that may
  *              run at the same time need one each.
  * fp16 dy: the q 2^e of a group are fp16 numbers times a power of two, which is one for the rows that a block sums and such that the largest is
- * finite (1 while q 2^e stay below 65,504, and then nothing of them is rounded; else what lies 2^39 below the largest is).
+ * finite (1 while magnitudes before the quantizer stay within 65,024, and then nothing of q 2^e is rounded; else what lies 2^39 below the largest is, and the block takes twice the time).
  * Accuracy: products are exact and summed on the tensor cores, which cut off what does not fit an fp32 sum.  fp32 results take the sums of at most
  * 1,024 rows (512 of fp16 dy) from there and add these in fp32; for 16-bit results up to 65,536 rows of bf16 or 16,384 of fp16 stay there, by which a
  * sum of one sign is too small by some 5e-5 of itself (measured).  Range: |q 2^e| below 2^127; sums of dy times rotated values are taken before H_G / G.
